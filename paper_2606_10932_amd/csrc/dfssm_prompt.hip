@@ -1147,7 +1147,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_scan(Args a) {
       // + M x.  M is the head's: each of its two waves prepares half of the tiles (rows
       // 16 rt .., tokens 32 s ..): those on the diagonal of 32 rows, and one below
       if (L::m_off == 0) arrive_lds();      // C is read
-      const int em = scale_exp(fmaxf(tok[kGMax] * tok[kDtMax], fabsf(Dh)));
+      // the diagonal adds D to its own C_i . B_i dt_i: the bound is that of the sum
+      const int em = scale_exp(tok[kGMax] * tok[kDtMax] + fabsf(Dh));
       const float sm = pow2(em);
       h8* Ms = reinterpret_cast<h8*>(lds + L::m_off + (v.id >> 1) * L::m_units * 1024) + v.lane;
       {
