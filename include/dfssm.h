@@ -475,7 +475,8 @@ dfssm_status dfssm_ssm_step_slots(const float* zxbcdt, int64_t ld, int64_t M, in
  *   y          [T, d_inner] fp32 out; must not overlap zxbcdt
  *   workspace  dfssm_ssm_prompt_workspace_bytes bytes; its contents do not
  *              matter and nothing stays in it, but calls that run at the same
- *              time need one each
+ *              time need one each.  The size does not fall as T or S grows: what
+ *              the largest call needs serves every smaller one
  * Limits: those of dfssm_ssm_step; ld <= 2^22; 0 <= T <= 2^24; 0 <= S <= 4096 (0 of
  * either is a no-op); S <= n_slots when slots is NULL.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED, DEVICE. */

@@ -1329,7 +1329,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_scan(Args a) {
 // ---------------------------------------------------------------- host
 struct Sizes {
   int64_t full, segments;      // chunks and segments of a sequence of all rows
-  int64_t chunks, segs, entries, splits;
+  int64_t chunks, segs, splits, entries;
+  int64_t table;               // room for segs that does not fall as T grows
 };
 
 // Segments of a sequence of all rows: such that they and the pairs of heads come to
@@ -1338,9 +1339,15 @@ struct Sizes {
 // more 85, with four or more 76), 16 at most.  Below six chunks prompt_ends and
 // prompt_starts cost more than they save: at 320 tokens 44 us whole and 50 split, at
 // 384 tokens 50 and 47.
-// The others are upper limits over every way to cut T rows into S sequences.  A split
-// sequence has more than full / segments chunks, so at least one more than `unit`, so
-// that its chunks are at most its rows / 64 (1 + 1 / unit).
+// The others are upper limits over every way to cut T rows into S sequences.  With f
+// chunks and g segments for all rows, f >= 2 g, a sequence of n chunks has ceil(n g / f)
+// segments, and s sequences have at most f + s - 1 chunks, so at most
+//   (sum of n g + s (f - 1)) / f <= g + s + ((s - 1) g - s) / f
+// segments; the last term is below (s - 1) / 2, so that is at most g + s - 1 + s / 2.
+// Split ones have more than f / g chunks each, so that there are no more than
+// f / floor(f / g) <= (3 g - 1) / 2 of them.  None of the limits that the workspace
+// follows falls as T or S grows, so that one made for the largest call serves every
+// smaller one.
 Sizes sizes(int64_t T, int64_t S, int64_t H) {
   Sizes z;
   const int64_t seqs = std::min(S, T);
@@ -1348,10 +1355,15 @@ Sizes sizes(int64_t T, int64_t S, int64_t H) {
   const int64_t fit = std::max<int64_t>(1, 512 / dfssm::ceil_div(H, kHeads));
   z.segments = z.full < 6 ? 1 : std::min({(int64_t)kMaxSegs, fit, z.full / 2});
   z.chunks = T / kChunk + seqs;
+  if (z.segments == 1) {
+    z.segs = z.table = seqs;
+    z.splits = z.entries = 0;
+    return z;
+  }
   z.segs = z.chunks * z.segments / z.full + seqs;
-  const int64_t unit = z.full / z.segments;
-  z.splits = z.segments > 1 ? z.full / unit : 0;
-  z.entries = z.segments > 1 ? dfssm::ceil_div((z.full + z.splits) * z.segments, z.full) + z.splits : 0;
+  z.table = z.segments + seqs + seqs / 2;      // segs is one below it at most
+  z.splits = std::min(seqs, (3 * z.segments - 1) / 2);
+  z.entries = z.segments + z.splits - 1 + z.splits / 2;
   return z;
 }
 
@@ -1370,7 +1382,7 @@ Carve carve(int64_t T, int64_t S, int64_t d_inner, int64_t N) {
   const Sizes z = sizes(T, S, H);
   Carve c;
   c.head = take(sizeof(Header));
-  c.segs = take((int64_t)sizeof(Seg) * z.segs);
+  c.segs = take((int64_t)sizeof(Seg) * z.table);
   c.splits = take(4 * z.splits);
   c.ops = take(z.chunks * (N == 128 ? Lay<128>::units : Lay<64>::units) * 1024);
   c.tok = take(z.chunks * H * kTokFloats * 4);

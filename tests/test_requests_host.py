@@ -81,6 +81,18 @@ def test_prompt_validation(dl):
     assert dl.ssm_prompt_workspace_bytes(1, 1, 64, 96) == 0
 
 
+@pytest.mark.parametrize("d_inner,N", [(64, 64), (1536, 128), (4096, 128), (5120, 64), (65536, 128)])
+def test_prompt_workspace_never_falls(dl, d_inner, N):
+    """A workspace for T rows and S sequences serves every smaller call."""
+    size = lambda T, S: dl.ssm_prompt_workspace_bytes(T, S, d_inner, N)
+    for S in (1, 2, 6, 33, 4096):
+        sizes = [size(T, S) for T in range(1, 9000)] + [size(T, S) for T in range(9000, 1 << 24, 99991)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), S
+    for T in (1, 64, 383, 384, 3008, 100000):
+        sizes = [size(T, S) for S in range(1, 4097)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), T
+
+
 def _adapt(dl, M=2, K=64, N=8, r=4, n=3, ids=16, A=16, B=16, be=16, y=16, out=16, ws=16, wsb=1 << 20, q=16, s=16, i4=False):
     f = dl.lib.dfssm_lora_adapters_i4 if i4 else dl.lib.dfssm_lora_adapters
     return f(q, s, M, K, N, r, ids, n, A, B, be, y, out, ws, wsb, None)
