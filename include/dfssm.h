@@ -501,7 +501,8 @@ dfssm_status dfssm_ssm_prompt(const float* zxbcdt, int64_t ld, int64_t T, const 
  *   _i4: A4 [n_adapters][r][K/2], B4 [n_adapters][N][r/2] bytes of packed
  *   int4 as for dfssm_scaffold_lora_linear_i4, r even
  *   workspace  dfssm_lora_adapters_workspace_bytes bytes, as dfssm_ssm_prompt's
- * Limits: K, M, N, r as for the linear, N <= 2^24 too; 0 <= n_adapters < 2^31
+ * Limits: K, M, N, r as for the linear, N <= 2^24 too, ceil(M / 64) *
+ * ceil(N / 256) < 2^24 and ceil(M / 64) * ceil(r / 16) < 2^23; 0 <= n_adapters < 2^31
  * (with no adapters or r == 0, A, B, beta, q, s and the workspace may be
  * NULL).  ids needs 4-byte alignment only.
  * Errors: NULL, SHAPE, ALIGN, WORKSPACE, DEVICE. */

@@ -808,8 +808,11 @@ dfssm_status lora_adapters(const int8_t* q, const float* s, int64_t M, int64_t K
   if (l4 && r % 2 != 0) return fail(DFSSM_ERR_SHAPE, "r=%lld must be even for packed int4 factors", (long long)r);
   if (N > (1 << 24)) return fail(DFSSM_ERR_SHAPE, "N=%lld must be <= 2^24", (long long)N);
   if (n_adapters < 0 || n_adapters > INT32_MAX) return fail(DFSSM_ERR_SHAPE, "n_adapters=%lld", (long long)n_adapters);
-  if (dfssm::ceil_div(M, 64) * dfssm::ceil_div(N, 256) > INT32_MAX)
-    return fail(DFSSM_ERR_SHAPE, "M=%lld rows of N=%lld are too many", (long long)M, (long long)N);
+  // workgroups of 256 threads, and of 512 that form acc_a: a launch has less than 2^32 threads
+  const int64_t windows = dfssm::ceil_div(M, 64);
+  if (windows * dfssm::ceil_div(N, 256) >= (1 << 24) || windows * dfssm::ceil_div(r, 16) >= (1 << 23))
+    return fail(DFSSM_ERR_SHAPE, "M=%lld rows of N=%lld at rank %lld are more than a launch can have", (long long)M,
+                (long long)N, (long long)r);
   if (M == 0 || N == 0) return DFSSM_OK;
   st = check_ptrs({{y, "y"}, {out, "out"}}, {});
   if (st != DFSSM_OK) return st;

@@ -121,6 +121,14 @@ def test_adapters_validation(dl, i4):
     assert dl.lora_adapters_workspace_bytes(-1, 4) == 0 and dl.lora_adapters_workspace_bytes(1, 257) == 0
 
 
+@pytest.mark.parametrize("i4", [False, True])
+def test_adapters_more_threads_than_a_launch_has(dl, i4):
+    # 2^19 windows of 64 rows by 16 tiles of ranks: 2^23 workgroups of 512 threads
+    assert _adapt(dl, M=1 << 25, r=256, N=1, wsb=1 << 62, i4=i4) == dl.ERR_SHAPE and "launch" in dl.last_error()
+    # 2^15 windows by 2^9 blocks of columns: 2^24 workgroups of 256
+    assert _adapt(dl, M=1 << 21, r=2, N=1 << 17, wsb=1 << 62, i4=i4) == dl.ERR_SHAPE and "launch" in dl.last_error()
+
+
 def test_odd_rank_int4(dl):
     assert _adapt(dl, r=3, i4=True) == dl.ERR_SHAPE and "even" in dl.last_error()
 
