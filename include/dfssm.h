@@ -446,8 +446,8 @@ dfssm_status dfssm_ssm_step(const float* zxbcdt, int64_t ld, int64_t M, int64_t 
 /* dfssm_ssm_step for one token of each of M requests, row m in slot slots[m]
  * at position positions[m]; the same roundings, so the same bits as
  * dfssm_ssm_step at that step.  y [M, d_inner] must not overlap zxbcdt.
- * Limits: those of dfssm_ssm_step; ld <= 2^22; 0 <= M <= 65536; 0 <= n_slots
- * < 2^31 (at 0 the pool may be NULL).
+ * Limits: those of dfssm_ssm_step; ld <= 2^22; 0 <= M <= 65536 and M * nheads <
+ * 2^24; 0 <= n_slots < 2^31 (at 0 the pool may be NULL).
  * Errors: NULL, SHAPE, ALIGN, UNSUPPORTED, DEVICE. */
 dfssm_status dfssm_ssm_step_slots(const float* zxbcdt, int64_t ld, int64_t M, int64_t d_inner, int64_t d_state,
                                   int64_t headdim, const int32_t* slots, const int32_t* positions,
