@@ -465,9 +465,22 @@ dfssm_status dfssm_ssm_step_slots(const float* zxbcdt, int64_t ld, int64_t M, in
  * and y's rows before the first or behind the last sequence are not written.
  * Offsets outside [0, T] or below an earlier one are raised or cut to the
  * nearest that is not.
- * The arithmetic is fp32, with sums in another order than the steps': per
- * element of y and of the state, the result is within rounding of theirs (a
- * few 2^-24 of the sum of the terms' magnitudes), not the same bits.  Results
+ * The arithmetic is fp32 with sums in another order than the steps', and its
+ * matrix products take each operand as two fp16 halves: not the same bits.  A
+ * value enters a product with an error of up to 2^-22 of itself, or 2^-39 of the
+ * largest value that shares an exponent with it where that is more (or 2^-85,
+ * where the largest is below 2^-46).  Rows are taken 64 at a time from the
+ * sequence's first on, and one exponent is shared by
+ *   B of 64 rows; C of 64 rows; a channel's x in 64 rows; a channel's state;
+ *   a head's exp(..) C_i . B_j dt_j (+ D) in 64 rows, whose largest is taken to
+ *   be max |C . B| max dt + |D|
+ * (rows behind the last count as repeating it in B and C, and as zeros before the
+ * convolution in x).  So where the values that share one lie within 2^17 of each
+ * other, an element of y or of the state is within rounding of the steps' (some
+ * 2^-24 of the sum of its terms' magnitudes), and else further off by up to 2^-39
+ * of the largest times what it is multiplied with: a row 2^30 times the others
+ * leaves those of its 64, earlier ones too, some 2^-9.  Nothing is promised where the
+ * product of two factors' largest values passes 2^155.  Results
  * are bitwise the same from run to run.  A row of a sequence with a value that
  * is not finite leaves nothing of use in the sequence's rows from up to 63
  * before it on, nor in its state; other sequences, and what a new one finds

@@ -99,6 +99,66 @@ def scan(zx, p, ring, state, pos, N):
                 state_rms=16 * U * habs + hsys + tiny)
 
 
+def wide(zx, p, ring, state, pos, N):
+    """What scan's bounds leave out: the prompts' products take an operand as fp16
+    halves under an exponent that it shares, so that beside 2^-22 of itself a value
+    is off by up to half of fp16's smallest step there, 2^-25 where the largest is
+    in [2^14, 2^15): 2^-39 of the largest, or 2^-85 (the exponent is 60 at most).
+    An exponent is shared by the B, and by the C, of 64 tokens, by a channel's x in
+    them, weighted or not, by a channel's state, and by a head's M in them, whose
+    largest is taken to be max |C . B| max dt + |D|.  Tokens behind the last one
+    count: their B and C repeat the last input, their x goes on from zeros.
+    Returns (y, state): bounds to add to scan's."""
+    f = lambda a: np.asarray(a, np.float64)
+    H = p["dt_bias"].shape[0]
+    di = 64 * H
+    cd = di + 2 * N
+    L = zx.shape[0]
+    zx, w, b, Dh = f(zx), f(p["conv_w"]), f(p["conv_b"]), np.abs(f(p["D"]))
+    h = np.zeros((H, 64, N)) if pos <= 0 else f(state).copy()
+    eh = np.zeros_like(h)
+    before = np.zeros((3, cd)) if pos <= 0 else f(ring)[[(pos + 1 + j) & 3 for j in range(3)]]
+    u = np.concatenate([before, zx[:, di:di + cd]])
+    dt_all = softplus(zx[:, di + cd:di + cd + H] + f(p["dt_bias"]))
+    A = -np.exp(f(p["A_log"]))
+    step = lambda m: np.maximum(1.01 * 2.0 ** -39 * m, 1.01 * 2.0 ** -85)
+    y_err = np.zeros((L, H, 64))
+    conv = lambda v: silu(b + sum(w[:, j] * v[j:j + 64] for j in range(4)))
+    for c0 in range(0, L, 64):
+        n = min(64, L - c0)
+        seg = u[c0:c0 + n + 3]
+        zeros = conv(np.concatenate([seg, np.zeros((64 - n, cd))]))
+        last = conv(np.concatenate([seg, np.repeat(seg[-1:], 64 - n, 0)]))
+        xg = zeros[:, :di].reshape(64, H, 64)
+        Bg, Cg = last[:, di:di + N], last[:, di + N:]
+        x, B, C, dt = xg[:n], np.abs(Bg[:n]), np.abs(Cg[:n]), dt_all[c0:c0 + n]
+        c = np.cumsum(dt * A, 0)
+        dB, dC = step(np.abs(Bg).max()), step(np.abs(Cg).max())
+        G = Cg @ Bg.T
+        tile = np.arange(64) // 16
+        gmax = np.abs(G[tile[:, None] >= tile]).max()
+        eG = dC * B.sum(1) + dB * C.sum(1)[:, None] + 2 * N * dB * dC                    # [i, j]
+        low = np.tril(np.ones((n, n)))
+        decay = np.exp(np.where(low > 0, c.T[:, :, None] - c.T[:, None, :], 0.0)) * low  # [H, i, j]
+        M = np.abs(decay * G[:n, :n] * dt.T[:, None]) + Dh[:, None, None] * np.eye(n)
+        eM = decay * eG * dt.T[:, None] + low * step(gmax * dt.max(0) + Dh)[:, None, None]
+        ax = np.abs(x).transpose(1, 0, 2)                                                # [H, j, p]
+        dx = step(np.abs(xg).max(0))                                                     # [H, p]
+        dM = step(gmax * dt.max(0) + Dh)
+        y1 = eM @ ax + M.sum(-1)[:, :, None] * dx[:, None] + 128 * dM[:, None, None] * dx[:, None]
+        ah = np.abs(h)
+        dh = step(ah.max(-1))
+        y2 = dC * ah.sum(-1)[:, None] + C.sum(1)[:, None] * dh[:, None] + 2 * N * dC * dh[:, None]
+        y2 = y2 + np.matmul(C, eh.transpose(0, 2, 1))
+        y_err[c0:c0 + n] = (y1 + np.exp(c.T)[:, :, None] * y2).transpose(1, 0, 2)
+        xw = (x * (dt * np.exp(c[-1] - c))[:, :, None]).transpose(1, 2, 0)               # [H, p, j]
+        dw = step(np.abs(xw).max(-1))
+        end = np.exp(c[-1])[:, None, None]
+        eh = end * eh + dw[..., None] * B.sum(0) + (np.abs(xw).sum(-1) * dB + 128 * dw * dB)[..., None]
+        h = end * h + xw @ Bg[:n]
+    return y_err.reshape(L, di), eh
+
+
 def assert_close(got, want, err, typical, what):
     got = np.asarray(got, np.float64)
     assert np.all(np.isfinite(got)), f"{what}: not finite"

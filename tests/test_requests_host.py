@@ -212,3 +212,15 @@ def test_bound_is_above_fp32_and_below_mistakes():
     for wrong in (dict(skip=0.999), dict(tap=0.0), dict(late=1)):
         with pytest.raises(AssertionError):
             R.assert_close(fp32(**wrong), ref["y"], ref["y_err"], ref["y_rms"], "wrong")
+
+
+def test_halves_cost_ordinary_inputs_nothing():
+    """Where no value is far above the others of its 64 tokens, what the halves of
+    the prompts' products lose under a shared exponent is lost in scan's bounds."""
+    rng = np.random.default_rng(7)
+    for H, N, L, pos in ((2, 64, 200, 5), (1, 128, 65, 0), (2, 128, 1, 3)):
+        p = _params(rng, H, N)
+        zx = rng.standard_normal((L, 2 * 64 * H + 2 * N + H)).astype(np.float32)
+        ring, state = rng.standard_normal((4, 64 * H + 2 * N)), 0.5 * rng.standard_normal((H, 64, N))
+        ref, (y, h) = R.scan(zx, p, ring, state, pos, N), R.wide(zx, p, ring, state, pos, N)
+        assert y.mean() <= 1e-4 * ref["y_err"].mean() and h.mean() <= 1e-4 * ref["state_err"].mean()
