@@ -293,9 +293,10 @@ __device__ __forceinline__ int scale_exp(float m) {
   return 141 - max(e, 81);
 }
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((127 + e) << 23); }
-// 2^-e for the sum of two of them: from 2^-120 up, and no further than to 2^127, where
-// the products of what they scale are past fp32, too.
-__device__ __forceinline__ float unscale(int e) { return pow2(min(-e, 127)); }
+// 2^-e for the sum of two of them: from 2^-120 up, and infinity from 2^128 on, where
+// the product of the largest values is past fp32 by 2^28: no finite value is wrong for
+// want of a second factor, which every sum would have to be multiplied with.
+__device__ __forceinline__ float unscale(int e) { return pow2(min(-e, 128)); }
 
 // Two products, a packed conversion, two v_fma_mix_f32 (what is left of a value, exact
 // since the scale is a power of two) and a packed conversion for two values: 23 clocks
