@@ -480,8 +480,13 @@ dfssm_status dfssm_ssm_step_slots(const float* zxbcdt, int64_t ld, int64_t M, in
  * 2^-24 of the sum of its terms' magnitudes), and else further off by up to 2^-39
  * of the largest times what it is multiplied with: a row 2^30 times the others
  * leaves those of its 64, earlier ones too, some 2^-9.  Where the product of
- * two factors' largest values passes 2^155, results may not be finite.  Results
- * are bitwise the same from run to run.  A row of a sequence with a value that
+ * two factors' largest values passes 2^155, results may not be finite.
+ * Results are bitwise the same from run to run.  The bits of a sequence follow
+ * from its rows, its slot's state and T (which decides where long sequences are
+ * split; up to 320 rows none is), and not from what else the T rows hold, S, or
+ * where its rows and slot lie; at another T they are others, within the same
+ * bounds.  So a server that pads its calls to one T gives a request the same bits
+ * in every batch.  A row of a sequence with a value that
  * is not finite leaves nothing of use in the sequence's rows from up to 63
  * before it on, nor in its state; other sequences, and what a new one finds
  * in its slot, are not touched by it.
