@@ -546,7 +546,7 @@ def _mixer_args(zxbcdt, conv_ring, ssm_state, conv_w, conv_b, dt_bias, A_log, D,
     if unit != 1 and cols > 1:
         raise ValueError("zxbcdt must have unit column stride")
     if rows < 2:      # a single row's stride may be reported as anything
-        ld = max(ld, cols)
+        ld = cols
     H, slots = dt_bias.shape[0], conv_ring.shape[0]
     d_inner = H * headdim
     conv_dim = d_inner + 2 * d_state
