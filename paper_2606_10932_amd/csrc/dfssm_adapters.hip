@@ -12,8 +12,9 @@
 // nothing has to be sorted.  Two launches: acc_a per row and rank, left in the
 // workspace as four signed base-256 digits, and the product with B with the
 // fp32 operations and y in its epilogue; or, for few rows, one that takes acc_a
-// itself.  Both the factors and y are read once, so bytes bound it from a few
-// hundred rows on: 7001 rows x 10576 columns at rank 16, 619 MB, adapter_down
+// itself.  y is read once, a factor once for each set of a window that names its
+// adapter (A once more per column block in that one launch), which is little beside
+// y where prompts make runs.  So bytes bound it from a few hundred rows on: 7001 rows x 10576 columns at rank 16, 619 MB, adapter_down
 // 10.5 and adapter_up 126 us (4.7 TB/s of y and out, a large copy's rate); below
 // that the launches and the round trips to memory do.
 #include <algorithm>
@@ -425,6 +426,18 @@ int window_parts(int64_t M, int64_t blocks, int64_t most) {
 //    9.4 / 10.3
 //  - int8 rank 64, 768 x 3352: 1 row 6.3 / 5.6; 2048 x 8512: 1 row 7.1 / 8.3
 //  - int4 rank 16, 768 x 3352: 1 row 7.0 / 5.2; rank 64: 6.8 / 7.0
+// and with ids in any order, up to 64 rows of 900 workgroups or fewer:
+//  - int8 rank 32, K 256 .. 2304: 6.0 .. 6.9 / 4.3 .. 6.7 at 1 row, 7.9 / 7.4 at 64 rows of
+//    2304 x 1152; K 4096: 8.0 / 8.6.  Rank 48, K 256 .. 1024: 5.9 .. 6.4 / 4.5 .. 5.5 at 1
+//    row; K 1536: 6.4 .. 7.4 / 6.4 .. 6.9; K 2048 and 2304: 6.9 / 7.2 .. 7.9.  Rank 64, K 1024:
+//    6.6 / 6.2 at 1 row, 7.5 / 8.9 at 16 of 4384 columns; K 1536: 6.7 / 7.3
+//  - int4 rank 32, K 256 .. 1024: 6.4 .. 6.9 / 5.0 .. 6.1 at 1 row; K 1536: 7.0 / 7.1.  Rank 48,
+//    K 512: 6.7 / 5.9; K 768: 6.9 / 6.4; K 1024: 6.9 / 6.9.  Rank 64, K 256: 6.6 / 5.6; K 512:
+//    6.8 / 6.3; K 768: 6.9 / 7.0
+//  - wrong by most near the limit of workgroups, where it depends on the ids: rank 16,
+//    4096 x 2048, 64 rows of one adapter 10.0 / 11.9, of 16 in runs 9.3 / 10.4, in any order
+//    9.0 / 9.7, in turn 8.4 / 7.2; 2048 x 8512, 16 rows of one adapter 7.7 / 6.1, in any order
+//    7.4 / 7.1, each its own 7.8 / 10.3, rank 32 7.7 / 9.1
 template <bool L4>
 bool few_is_best(const Args& a) {
   const int64_t tiles = a.rp / 16;

@@ -21,16 +21,19 @@
 //                  tables of the next launches), and prepares what all heads of a
 //                  chunk share: B and C after convolution and silu as MFMA operands,
 //                  C B^T, and per head dt, its decays and their sums
-//   prompt_ends    17, 52 us   only for sequences of more than one segment: each
+//   prompt_ends    18, 52 us   only for sequences of more than one segment: each
 //                  segment's final state from a zero state
 //   prompt_starts  12, 12 us   then turns those into the state before each segment
-//   prompt_scan    31, 108 us  walks each segment chunk by chunk with the state in
+//   prompt_scan    32, 109 us  walks each segment chunk by chunk with the state in
 //                  registers
 // A sequence of many chunks is split into segments where its heads alone would
-// leave most of the card idle.  72 and 188 us in all; one copy of what must be read
+// leave most of the card idle.  73 and 186 to 196 us in all; one copy of what must be read
 // and written would take 15 and 64 us.  What bounds them is the instructions of
-// prompt_scan and prompt_ends, not memory (1.0 and 1.6 TB/s): most of them turn
-// fp32 values into halves.
+// prompt_scan and prompt_ends, not memory (1.0 and 1.6 TB/s): of the 1460 vector
+// instructions of a chunk of prompt_scan beside its 228 MFMAs a third turn fp32
+// values into halves and a fifth convolve; of the 840 of prompt_ends beside 96 a
+// third convolve and a ninth make halves.  In 60 % of prompt_scan's clocks one is
+// issued; in the rest both waves of a SIMD wait for results, LDS or memory.
 #include <algorithm>
 #include <atomic>
 
@@ -483,7 +486,7 @@ constexpr int kDecayHeads = 32;
 template <int N>
 __device__ void chunk_decays(const Args& a, int c, const Place& p, int n, int h0, char* lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float* raw = reinterpret_cast<float*>(lds);  // [64 tokens][17]
+  float* raw = reinterpret_cast<float*>(lds);  // [64 tokens][kDecayHeads + 1]
   const float* z = a.zx + ((int64_t)p.row0 + p.k * kChunk) * a.ld + 2 * a.d_inner + 2 * N + h0;
   const int nh = min(kDecayHeads, a.H - h0);
   for (int i = tid; i < kChunk * kDecayHeads; i += kChunkThreads) {
@@ -990,7 +993,7 @@ __global__ __launch_bounds__(256) void prompt_starts(Args a, int elements, int s
 // A chunk: exp(c_i) C h and M while its inputs are on their way, then their convolution
 // and M x, and with B, which took the place of the last chunk's, the state's update, while
 // the next chunk's C, C B^T, tokens and inputs are asked for and the outputs stored.
-// 108 us at 7001 tokens of d_inner 5120.  A chunk is 3650 clocks of MFMA and 5300 of
+// 107 to 112 us at 7001 tokens of d_inner 5120.  A chunk is 3650 clocks of MFMA and 5300 of
 // other vector instructions for a wave, and the two waves of a SIMD hide little of the
 // one behind the other's: 75 us or more.  Preparing the operands of C h between its products
 // instead of before them changed nothing; x taken back from its halves for the update
@@ -1071,9 +1074,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_scan(Args a) {
     PHASE();
     const Taps taps = taps_of(a, v);      // kept over the chunk they would take ten registers
     PHASE();
-    decay = __builtin_amdgcn_exp2f(tok[kAll]);
+    decay = __builtin_amdgcn_exp2f(tok[kAll]);             // exp(c_64)
     eb = uniform(__float_as_int(tok[kEb]));
-    const int ec = uniform(__float_as_int(tok[kEc]));      // exp(c_64)
+    const int ec = uniform(__float_as_int(tok[kEc]));
     {
       // exp(c_i) C_i h, two row tiles and a k step at a time; operands read one ahead
 #pragma unroll
