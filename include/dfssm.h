@@ -471,7 +471,8 @@ dfssm_status dfssm_ssm_step_slots(const float* zxbcdt, int64_t ld, int64_t M, in
  * largest value that shares an exponent with it where that is more (or 2^-85,
  * where the largest is below 2^-46).  Rows are taken 64 at a time from the
  * sequence's first on, and one exponent is shared by
- *   B of 64 rows; C of 64 rows; a channel's x in 64 rows; a channel's state;
+ *   B of 64 rows; C of 64 rows; a channel's x in 64 rows, and again times dt and
+ *   its decay to the last row; a channel's state;
  *   a head's exp(..) C_i . B_j dt_j (+ D) in 64 rows, whose largest is taken to
  *   be max |C . B| max dt + |D|
  * (rows behind the last count as repeating it in B and C, and as zeros before the
